@@ -270,7 +270,8 @@ int fo_profile_end(fo_plan *plan, fo_kernel_time *out, size_t cap, size_t *count
  * inverse.  With FO_DITHER_UNIFORM u is an odd multiple of 2^-16 in (-1, 1), a function of (seed, round, party,
  * row * stride + coordinate), and the code's expectation over it is 127 y / max|y| to 2^-17: products of matrices coded
  * for different parties are unbiased, which is what the gradient oracle of Def. 3.1 asks of a gradient.
- * A row of zeros has amplitude 0 and codes 0; a row with an infinity or a NaN has amplitude NaN and codes 0.
+ * A row of zeros has amplitude 0 and codes 0; a row with an infinity or a NaN has amplitude NaN and codes 0.  Every finite row is coded: where
+ * the transform leaves fp32's range (sums of 2^block_log2 values), it is taken of 2^-16 of the row.
  * Arithmetic is fp32, the stages of a transform from the lowest coordinate bit up: the codes of a matrix and of its
  * transpose (`transposed`) are the same to the bit. */
 typedef struct {

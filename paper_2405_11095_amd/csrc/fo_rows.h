@@ -89,6 +89,7 @@ __device__ __forceinline__ uint32_t lane_sign(uint32_t lane, uint32_t block) // 
 }
 
 // Largest magnitude as the bits of a float: an infinity or a NaN is larger than every number
+constexpr uint32_t kInfinity = 0x7F800000u;
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t wave_max(uint32_t m) // in registers, the steps of wave_sum
 {
@@ -113,14 +114,14 @@ __device__ __forceinline__ RowFactor row_factor(uint32_t max_bits)
 {
     RowFactor f;
     const float m = __uint_as_float(max_bits);
-    f.finite = max_bits < 0x7F800000u;
+    f.finite = max_bits < kInfinity;
     f.up = m < 0x1p-64f ? 0x1p64f : 1.f;
     f.inv = f.finite && m > 0.f ? __fmul_rn(127.f, 1.f / (m * f.up)) : 0.f;
     return f;
 }
 __device__ __forceinline__ float row_scale(uint32_t max_bits, float unflatten)
 {
-    return max_bits < 0x7F800000u ? __uint_as_float(max_bits) * (1.f / 127.f) * unflatten : __builtin_nanf("");
+    return max_bits < kInfinity ? __uint_as_float(max_bits) * (1.f / 127.f) * unflatten : __builtin_nanf("");
 }
 
 // A code in the low byte: adding 1.5 2^23 rounds to the nearest integer, ties to even.  Without dither |127 y / max| is at most
@@ -144,6 +145,68 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
 }
 // u / 2 of 16 random bits: an odd multiple of 2^-17 in (-1/2, 1/2).  Sixteen bits bring E[q] within 2^-17 of a step of y.
 __device__ __forceinline__ float half_dither_of(uint32_t r16) { return (float)(int32_t)(2u * r16 + 1u - 65536u) * 0x1p-17f; }
+
+// Blocks of up to 2^10 finite values add up to as much as 2^138.  A row whose transform leaves fp32's range is transformed once more, 2^-16
+// of it (exact for whatever its codes can tell), by a workgroup of N threads, 1024 coordinates at a time in LDS, with the
+// same additions in the same order; x[k step] is its coordinate k.  Rare, and apart from the kernels' loops, where it would take 3 to 12 %
+// of their time.  Called by the whole workgroup; a row with an infinity or a NaN keeps what was written for it.
+template <typename T, uint32_t N>
+__device__ __forceinline__ void encode_lowered(const RowsArgs &a, const T *x, uint64_t step, uint64_t row, float *y, uint32_t *most)
+{
+    const uint32_t t = threadIdx.x;
+    const RngKey eps{ a.k0, a.k1, kDomainEps, a.round_lo, a.eps_party }, dither{ a.k0, a.k1, kDomainRowDither, a.round_lo, a.party };
+    uint32_t m = 0;
+    RowFactor f;
+    for (int pass = 0; pass < 2; ++pass) { // the largest magnitude, the codes
+        for (uint32_t k0 = 0; k0 < a.stride; k0 += 1024u) {
+            __syncthreads(); // y has been read
+            for (uint32_t i = t; i < 1024u; i += N) {
+                const uint32_t k = k0 + i;
+                uint32_t w[4];
+                philox(k / 128u, eps, w);
+                const uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3], low = k & 32u ? w1 : w0, high = k & 32u ? w3 : w2, n = k & 64u ? high : low;
+                y[i] = k < a.len ? flip_by_bit31(widen(x[k * step]) * 0x1p-16f, n << (31u - k % 32u)) : 0.f;
+            }
+            for (uint32_t b = 0; b < a.block; ++b) {
+                __syncthreads();
+                for (uint32_t p = t; p < 512u; p += N) {
+                    const uint32_t i = p >> b << (b + 1u) | (p & ((1u << b) - 1u)), j = i | 1u << b;
+                    const float u = y[i], v = y[j];
+                    y[i] = u + v;
+                    y[j] = u - v;
+                }
+            }
+            __syncthreads();
+            for (uint32_t i = 4u * t; i < 1024u && k0 + i < a.stride; i += 4u * N) {
+                if (pass == 0) {
+                    for (uint32_t c = 0; c < 4u; ++c) m = m > magnitude(y[i + c]) ? m : magnitude(y[i + c]);
+                    continue;
+                }
+                const uint64_t at = row * a.stride + k0 + i;
+                auto store = [&](uint32_t q0, uint32_t q1, uint32_t q2, uint32_t q3) {
+                    *reinterpret_cast<uint32_t *>(a.codes + at) = pack4(q0, q1, q2, q3);
+                };
+                if (a.dither) {
+                    uint32_t w[4];
+                    philox((uint32_t)(at >> 3), dither, w);
+                    const uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3], low = at & 4u ? w2 : w0, high = at & 4u ? w3 : w1;
+                    store(row_code(y[i], f.inv, half_dither_of(low & 0xFFFFu)), row_code(y[i + 1u], f.inv, half_dither_of(low >> 16)),
+                          row_code(y[i + 2u], f.inv, half_dither_of(high & 0xFFFFu)), row_code(y[i + 3u], f.inv, half_dither_of(high >> 16)));
+                } else {
+                    store(row_code(y[i], f.inv), row_code(y[i + 1u], f.inv), row_code(y[i + 2u], f.inv), row_code(y[i + 3u], f.inv));
+                }
+            }
+        }
+        if (pass) return;
+        m = wave_max(m);
+        if ((t & 63u) == 0u) most[t >> 6] = m;
+        __syncthreads();
+        for (uint32_t w = 0; w < N / 64u; ++w) m = m > most[w] ? m : most[w];
+        f = row_factor(m);
+        if (!f.finite) return;
+        if (t == 0) a.scales[row] = row_scale(m, a.unflatten) * 0x1p16f;
+    }
+}
 
 // A lane's 16 values of a segment, x[k] .. x[k + 7] and x[k + 512] .. x[k + 519], zero from `len` on, two (of 16 bits) or one in a
 // register.  (Where the whole segment lies in front of it both loads are on their way before either is waited for.)
@@ -194,7 +257,8 @@ struct Segment {
 template <typename T, int W, bool FEW>
 __global__ __launch_bounds__(W * 64) void k_rows_encode(const RowsArgs a)
 {
-    __shared__ __align__(16) uint32_t flips[FEW ? W * kRowSegment / 2 : (1u << 17) / 32]; // FEW: one for two coordinates; else bits
+    constexpr uint32_t kFlips = FEW ? W * kRowSegment / 2 : (1u << 17) / 32; // FEW: one for two coordinates; else bits
+    __shared__ __align__(16) uint32_t flips[kFlips < 1024u ? 1024u : kFlips];
     __shared__ uint32_t most[16];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     if (a.block) {
@@ -259,6 +323,7 @@ __global__ __launch_bounds__(W * 64) void k_rows_encode(const RowsArgs a)
         in.load(static_cast<const T *>(a.x) + row * a.ld, seg * kRowSegment + lane * 8u, (seg + 1u) * kRowSegment, a.len);
     };
 
+    uint32_t largest = 0; // over the rows
     if (FEW) load(blockIdx.x, wave);
     for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         uint32_t m = 0;
@@ -277,6 +342,7 @@ __global__ __launch_bounds__(W * 64) void k_rows_encode(const RowsArgs a)
 #pragma unroll
             for (int w = 0; w < W; ++w) m = m > most[w] ? m : most[w];
         }
+        largest = largest > m ? largest : m;
         const RowFactor f = row_factor(m);
         if (threadIdx.x == 0) a.scales[row] = row_scale(m, a.unflatten);
         const float inv = __uint_as_float(__float_as_uint(f.inv) ^ sign);
@@ -307,6 +373,11 @@ __global__ __launch_bounds__(W * 64) void k_rows_encode(const RowsArgs a)
             }
         }
     }
+    if (!a.block || __builtin_amdgcn_readfirstlane((int)largest) < (int)kInfinity) return;
+    __syncthreads(); // the amplitudes are there, the flips have been read
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x)
+        if (magnitude(a.scales[row]) > kInfinity)
+            encode_lowered<T, W * 64>(a, static_cast<const T *>(a.x) + row * a.ld, 1u, row, reinterpret_cast<float *>(flips), most);
 }
 
 // Columns of x as coded rows.  A workgroup takes C columns by 2^LOGK coordinates (C 2^(LOGK - 6) threads, 64 values each): a thread
@@ -431,10 +502,26 @@ __global__ __launch_bounds__(256) void k_columns_begin(float *scales, uint64_t r
     const uint64_t j = blockIdx.x * (uint64_t)256 + threadIdx.x;
     if (j < rows) scales[j] = 0.f;
 }
-__global__ __launch_bounds__(256) void k_columns_end(float *scales, uint64_t rows, float unflatten)
+// Maxima become amplitudes; columns whose transform left the range are coded here
+constexpr uint32_t kColumnsEnd = 64; // columns of a workgroup
+template <typename T>
+__global__ __launch_bounds__(256) void k_columns_end(const RowsArgs a)
 {
-    const uint64_t j = blockIdx.x * (uint64_t)256 + threadIdx.x;
-    if (j < rows) scales[j] = row_scale(__float_as_uint(scales[j]), unflatten);
+    __shared__ float y[1024];
+    __shared__ uint32_t most[4], list[kColumnsEnd], listed;
+    if (threadIdx.x == 0) listed = 0;
+    __syncthreads();
+    const uint64_t j = (uint64_t)blockIdx.x * kColumnsEnd + threadIdx.x;
+    if (threadIdx.x < kColumnsEnd && j < a.rows) {
+        const uint32_t m = __float_as_uint(a.scales[j]);
+        a.scales[j] = row_scale(m, a.unflatten);
+        if (m >= kInfinity) list[atomicAdd(&listed, 1u)] = threadIdx.x; // (each by itself, in any order)
+    }
+    __syncthreads();
+    for (uint32_t i = 0; i < listed && a.block; ++i) {
+        const uint64_t row = (uint64_t)blockIdx.x * kColumnsEnd + list[i];
+        encode_lowered<T, 256>(a, static_cast<const T *>(a.x) + row, a.ld, row, y, most);
+    }
 }
 
 } // namespace fo
