@@ -306,10 +306,12 @@ int fo_rows_product(const int8_t *a, const float *scales_a, uint64_t rows_a, con
  * bring every singular value towards 1; with the usual a, b, c = 3.4445, -4.7750, 2.0315 and five steps they end between 0.7 and
  * 1.2 unless they were tiny.  The products run on the matrix cores with fp32 sums; `products` says what the
  * iterates are rounded to between them:
- *   FO_PRODUCTS_HALF    fp16, scaled by 2^12: results are within about 1.5e-3 relative l2 for well conditioned updates, 2e-2 for ones
- *                       of rank one and 1 % noise (the map multiplies small singular directions, and the rounding in
- *                       them, by up to a^steps)
- *   FO_PRODUCTS_SINGLE  two fp16 parts (22 bits), three or four products instead of one: under 1e-6 and about 1e-5
+ *   FO_PRODUCTS_HALF    fp16, scaled by 2^12: results are within 4e-3 in relative l2 for well conditioned updates (about 1e-3 for large ones), 3e-2
+ *                       for ones of rank one and 1 % noise (the map multiplies small singular directions, and the
+ *                       rounding in them, by up to a^steps)
+ *   FO_PRODUCTS_SINGLE  two fp16 parts (22 bits), three or four products instead of one: within 2e-6 and 2e-5
+ * With fewer than eight rows or columns, whose few singular values the roundings do not average over, within 1e-2 and 5e-6 for
+ * well conditioned updates.  This is for five steps with the usual coefficients, at every size; the rounding of `out` to its type comes on top.
  * Iterates must stay below 16 in magnitude, which the usual coefficients ensure (other ones: infinities, then NaN).
  * The norm is formed in fp64.  A zero matrix gives zeros; one with an infinity or a NaN gives NaN everywhere. */
 #define FO_PRODUCTS_HALF 0u

@@ -332,6 +332,7 @@ struct Iterate {
 // A = X X^T
 template <bool TWO>
 struct GramEpilogue {
+    static constexpr bool sums_longer_than_sides = true;
     Iterate a;
     uint32_t side;
     template <int NQ, int NP>
@@ -357,6 +358,7 @@ __device__ __forceinline__ float polynomial(float a, float square, float ka, flo
 // B = a I + b A + c A^2
 template <bool TWO>
 struct PolyEpilogue {
+    static constexpr bool sums_longer_than_sides = false;
     Iterate a, b;
     uint32_t side;
     float ka, kb, kc; // ka times 2^12, kc times 2^-12
@@ -379,6 +381,7 @@ struct PolyEpilogue {
 // X <- B X
 template <bool TWO>
 struct UpdateEpilogue {
+    static constexpr bool sums_longer_than_sides = false;
     Iterate to;
     uint32_t rows, cols;
     template <int NQ, int NP>
@@ -397,6 +400,7 @@ struct UpdateEpilogue {
 // The last step's, into the caller's matrices, rows x cols, or turned where these are taller than wide: out = O, or x <- keep x - by O
 template <typename T, bool STEP, bool TALL>
 struct LastEpilogue {
+    static constexpr bool sums_longer_than_sides = false;
     MatrixTab out;
     uint64_t ld;
     uint32_t rows, cols; // of X without padding

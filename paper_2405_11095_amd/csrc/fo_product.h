@@ -10,9 +10,8 @@
 // the other; the one barrier of a stage stands in front of its second half step, whose fragments are in registers by then:
 // behind it the stage's buffer is free for the loads of the stage DEPTH further on, and the next stage has arrived.
 //
-// EXACT: operands in two parts of fp16 each.  The matrix cores round a sum after every eight products; with every stage it goes into a
-// second one and starts again at zero, which leaves a rounding of the whole sum every 64 products (orthogonalised updates of
-// 257 x 1025: off by 1.4e-6 with one every 256 and without the product of the second parts, 9e-7 so).
+// EXACT: operands in two parts of fp16 each.  The matrix cores round a sum after every eight products; with every run of stages it goes
+// into a second one and starts again at zero (kRun).
 //
 // P may come turned, its summed axis running down the columns (16-bit floats only): a stage of it is 64 rows of a tile's columns,
 // and its fragments are read through the LDS's transposing load, which hands lane c of 16 column c of 4 rows by 16 columns.
@@ -25,6 +24,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kStageBytes = 128;  // of a row, a stage
 constexpr uint32_t kMatrices = 64;     // matrices of one call
@@ -53,6 +53,14 @@ struct ProductArgs {
     uint32_t symmetric;       // Q = P: tiles on and above the diagonal only
     uint32_t count;           // matrices
 };
+
+// EXACT: a run is one stage as long as there are kShortSum of them, which leaves a rounding of the whole sum every 64 products (orthogonalised
+// updates of 257 x 1025: off by 1.4e-6 with one every 256 and without the product of the second parts, 9e-7 so).  In longer sums those
+// roundings would take over: a sum of n squares, all of one sign, is off by some sqrt(n / 64) half steps, and by n / 64 of them
+// where the squares are alike.  There a run is kRun stages, and what adding it to the second sum loses is taken into the next run
+// (in bf16: in fp32 it does not fit the registers of TileMid).  Off, in runs of one stage and so: 131072 x 32, 5.4e-6 and
+// 1.7e-6; 4 x 524288 of +-1, 8e-4 and 4e-6; in the same time (32 x 131072 4.8 ms, 4096 x 11008 12.0, 6000 x 6000 15.8 and 15.4).
+constexpr uint32_t kShortSum = 64, kRun = 8;
 
 // The tile of a workgroup.  Workgroups go round the eight XCDs, each with an L2 of its own: each gets a contiguous run of the
 // tiles instead, and a run goes down bands of eight tiles, whose operands the L2 holds.
@@ -144,7 +152,8 @@ __device__ __forceinline__ void trade(f32x4 &a, f32x4 &b, int r)
 
 // Epi: void operator()(const TileAt &, uint32_t q, uint32_t p, const Acc (&)[NQ][NP]): the lane's outputs, of which element r of
 // [i][j] is (q + i, p + 4 j + r); rows past the matrices' ends are among them
-template <typename Op, typename Shape, bool TURNED, bool EXACT, typename Epi>
+// RUNS: EXACT in runs of more than one stage
+template <typename Op, typename Shape, bool TURNED, bool EXACT, bool RUNS, typename Epi>
 __global__ __launch_bounds__(Shape::threads, 2) void k_product(const ProductArgs a, const Epi epi)
 {
     constexpr int NQ = Shape::NQ, NP = Shape::NP, PARTS = Shape::PARTS;
@@ -209,6 +218,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void k_product(const ProductArgs
     }
     i32x4 fq[2][PARTS][NQ], fp[2][PARTS][NP];
     Acc acc[NQ][NP] = {}, low[PARTS == 2 ? NQ : 1][NP] = {}, sum[EXACT ? NQ : 1][NP] = {}; // low: the products with second parts
+    bf16x4 lost[RUNS ? NQ : 1][NP] = {};
     uint32_t column[NP]; // turned: where the 16 columns of a fragment lie in a row
 #pragma unroll
     for (int i = 0; i < NP; ++i) column[i] = ((wp / 16u + i) ^ swizzle_turned<Shape>(8u * (lane >> 4) + (lane >> 2 & 3u))) << 5;
@@ -246,7 +256,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void k_product(const ProductArgs
             });
 #pragma unroll
             for (int j = 0; j < NP; ++j) {
-                if constexpr (EXACT && H == 0) { // sums start anew with every stage
+                if constexpr (EXACT && !RUNS && H == 0) { // sums start anew with every stage
                     sum[i][j] += acc[i][j];
                     acc[i][j] = Op::mfma(fp[H][0][j], fq[H][0][i], Acc{});
                 } else {
@@ -285,9 +295,25 @@ __global__ __launch_bounds__(Shape::threads, 2) void k_product(const ProductArgs
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kReads; ++i) read(0, 0, i);
-    uint32_t buffer = 0;
+    uint32_t buffer = 0, left = (a.segments - 1u) * a.stages + kRun; // (what second parts add is small, and goes with the first run)
+    auto run = [&]() {
+        if constexpr (RUNS) {
+            if (left-- != 0u) return;
+            left = kRun - 1u;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+#pragma unroll
+                for (int j = 0; j < NP; ++j) {
+                    const Acc add = acc[i][j] - __builtin_convertvector(lost[i][j], Acc), to = sum[i][j] + add;
+                    lost[i][j] = __builtin_convertvector((to - sum[i][j]) - add, bf16x4);
+                    sum[i][j] = to;
+                    acc[i][j] = Acc{};
+                }
+        }
+    };
     auto follow = [&](uint32_t b) { return b + kBuffer == D * kBuffer ? 0u : b + kBuffer; };
     for (uint32_t s = D; s < total; ++s) {
+        run();
         half(first, buffer, std::false_type{}, 0);
         loads_done<(D - 2) * each>();
         __syncthreads();
@@ -296,6 +322,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void k_product(const ProductArgs
         buffer = follow(buffer);
     }
     for (uint32_t s = total < (uint32_t)D ? total : D; s; --s) { // nothing left to load; what the very last half step reads is not used
+        run();
         half(first, buffer, std::false_type{}, 0);
         loads_done<0>();
         __syncthreads();
@@ -307,6 +334,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void k_product(const ProductArgs
         for (int i = 0; i < NQ; ++i)
 #pragma unroll
             for (int j = 0; j < NP; ++j) {
+                if constexpr (RUNS) acc[i][j] -= __builtin_convertvector(lost[i][j], Acc);
                 if constexpr (PARTS == 2) acc[i][j] += low[i][j];
                 acc[i][j] += sum[i][j];
             }
@@ -365,14 +393,20 @@ inline uint64_t product_tiles(const ProductArgs &a, uint32_t side)
     return a.count * (a.symmetric ? q * (q + 1u) / 2u : q * p);
 }
 
-template <typename Op, bool TURNED, bool EXACT, typename Shape, typename Epi>
+template <typename Op, bool TURNED, bool EXACT, typename Shape, bool RUNS = false, typename Epi>
 void launch_product_as(ProductArgs a, const Epi &epi, hipStream_t st)
 {
     a.segments = EXACT && Shape::PARTS == 1 ? 3u : 1u; // EXACT: operands in two parts
     static_assert(Shape::Q == Shape::P, "the upper triangle of a symmetric product is one of square tiles");
     a.tiles_q = (a.rows_q + Shape::Q - 1u) / Shape::Q;
     a.tiles_p = (a.rows_p + Shape::P - 1u) / Shape::P;
-    hipLaunchKernelGGL((k_product<Op, Shape, TURNED, EXACT, Epi>), dim3((unsigned)product_tiles(a, Shape::Q)), dim3(Shape::threads), 0, st, a, epi);
+    const dim3 grid((unsigned)product_tiles(a, Shape::Q)), block(Shape::threads);
+    if constexpr (RUNS)
+        if (a.stages > kShortSum) {
+            hipLaunchKernelGGL((k_product<Op, Shape, TURNED, EXACT, true, Epi>), grid, block, 0, st, a, epi);
+            return;
+        }
+    hipLaunchKernelGGL((k_product<Op, Shape, TURNED, EXACT, false, Epi>), grid, block, 0, st, a, epi);
 }
 template <typename Op, bool TURNED = false, bool EXACT = false, typename Epi>
 void launch_product(const ProductArgs &a, const Epi &epi, hipStream_t st)
@@ -385,9 +419,12 @@ void launch_product(const ProductArgs &a, const Epi &epi, hipStream_t st)
         //   300   1500 x 1500 x 1500, upper half             31     24     31
         //   528   2000 x 2000 x 2000, upper half      58            54     59
         //   528   1000 x 2050 x 1000                  30            29     34
-        if (product_tiles(a, 128u) >= 256u) launch_product_as<Op, TURNED, EXACT, TileMid>(a, epi, st);
-        else if (product_tiles(a, 64u) > 256u) launch_product_as<Op, TURNED, EXACT, TilePairs>(a, epi, st);
-        else launch_product_as<Op, TURNED, EXACT, TilePairsDeep>(a, epi, st);
+        // A sum longer than kShortSum over few outputs is one of Gram's: in the other products it is no longer than either side.
+        constexpr bool longer = Epi::sums_longer_than_sides;
+        static_assert(33u * 34u / 2u >= 256u, "upper half of the least sides, 65 stages, in tiles of 128");
+        if (product_tiles(a, 128u) >= 256u) launch_product_as<Op, TURNED, EXACT, TileMid, true>(a, epi, st);
+        else if (product_tiles(a, 64u) > 256u) launch_product_as<Op, TURNED, EXACT, TilePairs, longer>(a, epi, st);
+        else launch_product_as<Op, TURNED, EXACT, TilePairsDeep, longer>(a, epi, st);
     } else {
         if constexpr (!TURNED)
             if (product_tiles(a, 128u) > 512u && product_tiles(a, 192u) <= 256u) return launch_product_as<Op, TURNED, EXACT, TileLarge>(a, epi, st);
