@@ -339,8 +339,8 @@ void fo_matrix_plan_destroy(fo_matrix_plan *plan);
 size_t fo_matrix_scratch_bytes(const fo_matrix_plan *plan);
 
 /* out[i] = the orthogonalised g[i], i < count.  g, out: HOST arrays of count device pointers, each [rows][ld]; out[i]
- * may be g[i] itself (with ld_out = ld_g); other overlaps are not allowed (FO_EINVAL where two start at one address).  FO_EINVAL also
- * if the current device is not the plan's. */
+ * may be g[i] itself (with ld_out = ld_g).  FO_EINVAL if an output overlaps anything else (matrices side by side in a larger one do not
+ * overlap), or if the current device is not the plan's. */
 int fo_orthogonalize(fo_matrix_plan *plan, const void *const *g, uint64_t ld_g, void *const *out, uint64_t ld_out, void *hip_stream);
 
 /* One step of momentum and orthogonalised update on the plan's matrices, each a contiguous [rows][cols]:

@@ -174,6 +174,27 @@ bool apart(Range *r, uint32_t n)
     return true;
 }
 
+// Whether two matrices have memory in common: `rows` rows of `bytes` each, which follow one another after step_a or step_b bytes.
+// (Matrices may lie side by side in a larger one, so that their stretches of memory alone do not tell.)
+bool meet(uintptr_t a, uint64_t step_a, uintptr_t b, uint64_t step_b, uint64_t rows, uint64_t bytes)
+{
+    const uint64_t last_a = (rows - 1u) * step_a, last_b = (rows - 1u) * step_b;
+    if (a + last_a + bytes <= b || b + last_b + bytes <= a) return false;
+    const int64_t from = (int64_t)(a - b), end = (int64_t)(last_b + bytes), step = (int64_t)step_b, row = (int64_t)bytes;
+    if (step_a == step_b) { // the rows of a lie in the rows of b all in the same way
+        const int64_t in = ((from % step) + step) % step, down = (from - in) / step, most = (int64_t)rows - 1;
+        return (in < row && down >= -most && down <= most) || (in + row > step && down + 1 >= -most && down + 1 <= most);
+    }
+    for (uint64_t i = 0; i < rows; ++i) {
+        const int64_t x = from + (int64_t)(i * step_a);
+        if (x <= -row) continue;
+        if (x >= end) return false;
+        const int64_t in = ((x % step) + step) % step;
+        if (in < row || in + row > step) return true;
+    }
+    return false;
+}
+
 int on_device(const fo_matrix_plan *pl)
 {
     int dev = -1;
@@ -251,10 +272,12 @@ extern "C" int fo_orthogonalize(fo_matrix_plan *pl, const void *const *g, uint64
     Last last;
     FO_TRY(take(pl, g, size, from));
     FO_TRY(take(pl, out, size, last.out));
+    const uint64_t rows = pl->p.rows, bytes = pl->p.cols * size, step_g = ld_g * size, step_out = ld_out * size;
     for (uint32_t i = 0; i < pl->p.count; ++i)
         for (uint32_t j = 0; j < pl->p.count; ++j) {
-            if (j < i && out[i] == out[j]) return FO_EINVAL;
-            if (out[i] == g[j] && (i != j || ld_g != ld_out)) return FO_EINVAL;
+            const uintptr_t o = reinterpret_cast<uintptr_t>(out[i]), o2 = reinterpret_cast<uintptr_t>(out[j]), x = reinterpret_cast<uintptr_t>(g[j]);
+            if (j < i && meet(o, step_out, o2, step_out, rows, bytes)) return FO_EINVAL;
+            if (!(i == j && o == x && ld_g == ld_out) && meet(o, step_out, x, step_g, rows, bytes)) return FO_EINVAL;
         }
     FO_TRY(on_device(pl));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
