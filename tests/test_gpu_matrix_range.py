@@ -1,7 +1,7 @@
-"""Orthogonalised updates at the ends of their range: long sides."""
+"""Orthogonalised updates at the ends of their range: long sides, overlaps, values that are no numbers, few steps and many."""
 import pytest
 
-from tests.test_gpu_matrix import env, exactly, update  # noqa: F401
+from tests.test_gpu_matrix import COEFFICIENTS, check, env, exactly, update  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +69,64 @@ def test_outputs_that_meet_anything_else_are_refused(env):
     with pytest.raises(B.FoError):
         one.fo_orthogonalize([flat[None, 0:12]], [flat[None, 11:23]])
     one.fo_orthogonalize([flat[None, 0:12]], [flat[None, 12:24]])
+
+
+BOTH_PATHS = [(40, 70), (70, 40), (1, 9), (128, 128), (150, 200), (200, 150), (300, 1), (129, 129)]  # in one workgroup up to 128 x 128
+
+
+@pytest.mark.parametrize("dtype,single", [("float32", True), ("float32", False), ("bfloat16", False), ("float16", True)])
+@pytest.mark.parametrize("rows,cols", BOTH_PATHS)
+def test_any_magnitude_zero_and_no_numbers_side_by_side(env, rows, cols, dtype, single):
+    """What one matrix of a call holds is its own affair, on either path: a power of two changes no bit, zeros stay zeros, and an infinity
+    or a NaN spoils its own matrix everywhere and no other."""
+    B, torch = env
+    dt = getattr(torch, dtype)
+    kw = dict(dtype=dt, products=B.PRODUCTS_SINGLE if single else B.PRODUCTS_HALF)
+    up, down = (2.0 ** 9, 1.0) if dtype == "float16" else (2.0 ** 120, 2.0 ** -100)       # (fp16 has no room below)
+    g = torch.stack([update(torch, rows, cols, 1).to(dt).float() * f for f in (1, up, down, 0, 1, 1, 1, 1)]).to(dt)
+    g[4, rows // 2, cols // 2], g[5, 0, 0], g[6, rows - 1, cols - 1] = float("nan"), float("inf"), -float("inf")
+    out = torch.empty_like(g)
+    B.MatrixPlan(rows, cols, count=8, **kw).fo_orthogonalize(g, out)
+    assert bool(out[0].isfinite().all()) and bool(out[0].any())
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2]) and torch.equal(out[0], out[7]) and not bool(out[3].any())
+    assert bool(out[4:7].isnan().all())
+
+
+@pytest.mark.parametrize("nesterov", (False, True))
+@pytest.mark.parametrize("rows,cols", BOTH_PATHS)
+def test_steps_with_zeros_and_no_numbers_side_by_side(env, rows, cols, nesterov):
+    """A step of a normal gradient beside one of zeros (parameters decay, nothing else), zeros with a momentum, a NaN and an infinity."""
+    B, torch = env
+    kw = dict(nesterov=nesterov, scale=2.0, decay=0.1)
+    g = torch.stack([update(torch, rows, cols, k) for k in range(5)])
+    m = torch.stack([update(torch, rows, cols, 10 + k) for k in range(5)])
+    x = torch.stack([update(torch, rows, cols, 20 + k) * 20 for k in range(5)])
+    g[1:3] = 0
+    m[1] = 0
+    g[3, rows - 1, 0], g[4, 0, cols - 1] = float("nan"), -float("inf")
+    m1, x1 = m.clone(), x.clone()
+    B.MatrixPlan(rows, cols, count=5).fo_matrix_step(g, m1, x1, 0.02, **kw)
+    one = B.MatrixPlan(rows, cols)
+    for k in (0, 2):
+        mk, xk = m[k].clone(), x[k].clone()
+        one.fo_matrix_step([g[k]], [mk], [xk], 0.02, **kw)
+        assert torch.equal(m1[k], mk) and bool(x1[k].isfinite().all())
+        # (one matrix may take other tiles, whose sums are in another order)
+        assert float((x1[k].double() - xk.double()).norm()) <= 1e-5 * float((xk.double() - x[k].double()).norm())
+    f32 = torch.tensor
+    keep = f32(1.0 - float(f32(0.02, dtype=torch.float32)) * float(f32(0.1, dtype=torch.float32)), dtype=torch.float32).cuda()
+    assert not bool(m1[1].any()) and torch.equal(x1[1], x[1] * keep)
+    for k, bad in ((3, g[3].isnan()), (4, g[4].isinf())):
+        assert torch.equal(m1[k].isfinite(), ~bad) and bool(x1[k].isnan().all())
+
+
+@pytest.mark.parametrize("rows,cols", [(100, 70), (70, 100), (128, 128), (1, 50), (33, 31), (150, 100)])
+def test_steps_and_coefficients_of_either_orientation(env, rows, cols):
+    B, torch = env
+    g = update(torch, rows, cols, 1)
+    for steps, k in ((1, COEFFICIENTS), (2, COEFFICIENTS), (3, (2.0, -1.5, 0.5)), (12, (1.875, -1.25, 0.375)), (16, (1.5, -0.5, 0.0))):
+        for single in (False, True):
+            plan = B.MatrixPlan(rows, cols, products=int(single), steps=steps, coefficients=k)
+            out = torch.empty_like(g)
+            plan.fo_orthogonalize([g], [out])
+            check(torch, out, g, single, f"{steps} steps", steps=steps, coefficients=k)

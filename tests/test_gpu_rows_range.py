@@ -1,8 +1,9 @@
-"""8-bit rows over fp32's whole range: rows of finite values whose transform leaves it."""
+"""8-bit rows at the ends of their range: finite values whose transform leaves fp32's, codes that saturate."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_rows import ROUND, SEED, _check_codes, _dithers, _signs, env  # noqa: F401
+from tests.row_codes import off_from_definition
+from tests.test_gpu_rows import CASES, ROUND, SEED, TYPES, _check_codes, _dithers, _flattened, _matrix, _signs, env  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +60,19 @@ def test_their_neighbours_keep_their_codes(env, turned):
     assert torch.equal(s[(kind != 1) & ~bad], alone[1][(kind != 1) & ~bad])
     want = alone[1][kind == 1].double() * 2.0 ** 125
     assert bool(((s[kind == 1].double() - want).abs() <= 2.0 ** -23 * want).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,length,block,pad,dither", CASES)
+def test_saturated_codes_too(env, oracle, rows, length, block, pad, dither, dtype):
+    """Every code against its definition, those at the ends of the range with their sign and on ragged tails."""
+    B, torch = env
+    x = _matrix(torch, rows, length, getattr(torch, dtype), pad, rows + length + 1)
+    stride = B.fo_rows_stride(length, block)
+    y, total = _flattened(x.double().cpu().numpy(), stride, block, _signs(oracle, stride) if block else None)
+    u = _dithers(oracle, rows, stride, 11) if dither else np.zeros((rows, stride))
+    for turned in (False, True):
+        q, s = _encode(B, torch, x, block, turned, dither)
+        q = q.cpu().numpy().astype(np.float64)
+        assert np.all(off_from_definition(q, y, total, u, block) <= 0)
+        assert np.all(np.abs(q).max(axis=1)[np.abs(y).max(axis=1) > 0] == 127)
