@@ -268,8 +268,9 @@ int fo_profile_end(fo_plan *plan, fo_kernel_time *out, size_t cap, size_t *count
  * row.  eps is one stream for everybody (as in FO_EPS_SHARED_ALL) and depends on (seed, round, coordinate of the row): the
  * transforms of two matrices coded with the same seed, round and block_log2 cancel in their product, which needs no
  * inverse.  With FO_DITHER_UNIFORM u is an odd multiple of 2^-16 in (-1, 1), a function of (seed, round, party,
- * row * stride + coordinate), and the code's expectation over it is 127 y / max|y| to 2^-17: products of matrices coded
- * for different parties are unbiased, which is what the gradient oracle of Def. 3.1 asks of a gradient.
+ * row * stride + coordinate), and the code's expectation over it is 127 y / max|y| to about 2^-15 of a step, with y as fp32 gives it (u has 16
+ * bits; the factor and the product with it round three times, by 2^-24 of up to 127): products of matrices coded for
+ * different parties are unbiased to that, which is what the gradient oracle of Def. 3.1 asks of a gradient.
  * A row of zeros has amplitude 0 and codes 0; a row with an infinity or a NaN has amplitude NaN and codes 0.  Every finite row is coded: where
  * the transform leaves fp32's range (sums of 2^block_log2 values), it is taken of 2^-16 of the row.
  * Arithmetic is fp32, the stages of a transform from the lowest coordinate bit up: the codes of a matrix and of its

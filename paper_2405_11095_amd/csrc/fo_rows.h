@@ -143,7 +143,8 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
 {
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
-// u / 2 of 16 random bits: an odd multiple of 2^-17 in (-1/2, 1/2).  Sixteen bits bring E[q] within 2^-17 of a step of y.
+// u / 2 of 16 random bits: an odd multiple of 2^-17 in (-1/2, 1/2).  Sixteen bits bring E[q] within 2^-17 of what is rounded, which itself is off
+// from 127 y / max by three roundings of 2^-24 of up to 127 (2^-15.4 at most, found over all 2^16 dithers of 4000 values).
 __device__ __forceinline__ float half_dither_of(uint32_t r16) { return (float)(int32_t)(2u * r16 + 1u - 65536u) * 0x1p-17f; }
 
 // Blocks of up to 2^10 finite values add up to as much as 2^138.  A row whose transform leaves fp32's range is transformed once more, 2^-16
