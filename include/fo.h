@@ -267,7 +267,9 @@ int fo_profile_end(fo_plan *plan, fo_kernel_time *out, size_t cap, size_t *count
  * so that scales[r] * codes is the flattened row (Def. 3.5) up to rounding: an outlier column no longer sets the step of its
  * row.  eps is one stream for everybody (as in FO_EPS_SHARED_ALL) and depends on (seed, round, coordinate of the row): the
  * transforms of two matrices coded with the same seed, round and block_log2 cancel in their product, which needs no
- * inverse.  With FO_DITHER_UNIFORM u is an odd multiple of 2^-16 in (-1, 1), a function of (seed, round, party,
+ * inverse.  It is the very stream that an FO_EPS_SHARED_* plan of the same seed draws in that round: where such a plan takes a
+ * gradient made of these products, give the rows another seed, or the gradient depends on the signs that then flatten it
+ * (plans of FO_EPS_INDEPENDENT draw others for every party).  With FO_DITHER_UNIFORM u is an odd multiple of 2^-16 in (-1, 1), a function of (seed, round, party,
  * row * stride + coordinate), and the code's expectation over it is 127 y / max|y| to about 2^-15 of a step, with y as fp32 gives it (u has 16
  * bits; the factor and the product with it round three times, by 2^-24 of up to 127): products of matrices coded for
  * different parties are unbiased to that, which is what the gradient oracle of Def. 3.1 asks of a gradient.
