@@ -223,7 +223,7 @@ extern "C" int fo_matrix_plan_create(const fo_matrix_params *params, fo_matrix_p
     pl->m64 = (uint32_t)((m + 63u) & ~(uint64_t)63u);
     pl->n64 = (uint32_t)((n + 63u) & ~(uint64_t)63u);
     pl->parts = q.products == FO_PRODUCTS_SINGLE ? 2u : 1u;
-    const uint64_t work = (m * n + 2047u) / 2048u; // a vector a thread
+    const uint64_t work = (m * n + 2047u) / 2048u; // a unit of two vectors of fp32 a thread (16-bit ones need half the workgroups)
     pl->nparts = (uint32_t)(work < 1024u ? work : 1024u);
     if (!hip_ok(hipGetDevice(&pl->device), "hipGetDevice")) {
         delete pl;

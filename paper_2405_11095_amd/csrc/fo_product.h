@@ -103,7 +103,8 @@ struct TileShape {
 // Which row of an operand stands at place m (0 .. 15) of fragment n is free.  Rows of Q go to fragments so that the NQ fragments
 // of a wave hold, at place m, NQ neighbouring rows, m NQ ..; rows of P so that the four places 4 g .. 4 g + 3 of all NP fragments,
 // which are the outputs of lane group g, hold 4 NP neighbouring rows.  A lane's outputs then are a block of NQ by 4 NP, and are
-// stored along either side in whole vectors.  (Scalar stores of the transposed half: 11008 x 4096 in fp16, update product 392 us.)
+// stored along either side in whole vectors.  (Scalar stores of the transposed half: 11008 x 4096 in fp16, update product 392 us,
+// 355 so.)
 // In LDS a fragment's rows follow one another; row `at` of the stage there is this row of the tile:
 template <int N>
 __device__ __forceinline__ uint32_t row_q(uint32_t at) { return at / (16u * N) * (16u * N) + at % 16u * N + at / 16u % N; }
@@ -114,7 +115,7 @@ __device__ __forceinline__ uint32_t swizzle(uint32_t r, uint32_t c) { return r *
 
 // Turned, columns stay in their order, 16 neighbours a fragment, and lane group g's outputs are columns 4 g .. 4 g + 3 of every 16;
 // lane groups trade them in the end, for blocks of neighbours as above.  A transposing load takes 32 lanes at once: 32 bytes of eight rows, k & 3 and bit 3 of k.  The rows move them to 32-byte pieces of
-// their own.  (Columns in blocks of 4 NP as above would read half of every 16 bytes: 11008 x 4096, update product 399 us.)
+// their own.  (Columns in blocks of 4 NP as above would read half of every 16 bytes: 11008 x 4096, update product 399 us, 329 so.)
 template <typename Shape>
 __device__ __forceinline__ uint32_t swizzle_turned(uint32_t k)
 {
@@ -125,7 +126,7 @@ __device__ __forceinline__ uint32_t swizzle_turned(uint32_t k)
 // 16 bytes a lane from a base that is the same in every lane, plus a lane's offset, to LDS address `lds` + 16 x lane.  In assembly,
 // since in front of a read from LDS the compiler waits for all such loads of its own making wherever it cannot tell their
 // addresses apart (transposing reads; a second object in LDS), which takes the prefetch away: 11008 x 4096, update product
-// 283 -> 380 us.  It has no output to be overwritten; loads_done() waits for it.  The wait states are those between M0 and the load
+// 381 us, 323 so.  It has no output to be overwritten; loads_done() waits for it.  The wait states are those between M0 and the load
 // (1) and between a base from the vector unit and the load (5).
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t lds)
 {
@@ -359,23 +360,25 @@ __global__ __launch_bounds__(Shape::threads, 2) void k_product(const ProductArgs
 
 // ---- which tile ----------------------------------------------------------------------------------------------------------------
 // A compute unit holds one workgroup of TileBig or TileLarge, two of TileMid or TileDeep, five of TileSmall.  What bounds a stage is
-// the way from the L2 to LDS, 25 bytes a cycle and compute unit or so: large tiles move the fewest bytes for an output, small ones
-// use more of the 256 units.  us, fp16 (i8 where said):
+// the way from the L2 to LDS, at 2.4 GHz some 19 bytes a cycle and compute unit with one workgroup (Large, 4096 x 4096 x 11008) and 24 to 33 with
+// five (4096 x 4096 x 4096): large tiles move the fewest bytes for an output, small ones use more of the 256 units.
+// us, each kernel by itself in a trace, fp16 (i8 where said); full products are those down the columns:
 //   tiles of 256 / 192 / 128 sides                    Big   Large   Mid  Small  Deep
-//   256 / 484 / 1024   4096 x 4096 x 4096             102           122   182    196
-//   136 / 253 / 528    the same, upper half            81            96   126    155
-//   136 / 253 / 528    4096 x 4096 x 11008, upper half 235    199
-//   192 / 432 / 768    12 of 1024 x 1024 x 1024        28            31    38     44
-//   144 / 231 / 544    4000 x 2064 x 16384, i8        177    135    182   224    217
-//   120 / 252 / 432    12 of 1024, upper halves        25     28     18    23     25
-//    80 / 168 / 288    8 of 1024 x 1024 x 4096, upper halves  75     65
-//    66 / 120 / 253    2800 x 2800 x 8192, upper half                90   110
-//    45 /  78 / 171    2300 x 2300 x 8192, upper half                82    78
-//    64 / 121 / 256    2048 x 2048 x 2048              42            26    25     27
-//    36 /  66 / 136    2048, upper half                42            23    20     23
-//    32 /  66 / 128    512 x 4096 x 4096, i8           42            20    16     15
-//    10 /  21 /  36    1024 x 1024 x 6336, upper half 112            64    49     27
-//    56 /  75 / 112    77 x 14336 x 4096, i8           39            24    19     14
+//   688 /    - / 2752  4096 x 11008 x 4096            303           354   521   548
+//   256 /    - / 1024  4096 x 4096 x 4096             118           148   210   236
+//   136 / 253 / 528    the same, upper half            98     88    109   147   160
+//   136 / 253 / 528    4096 x 4096 x 11008, upper half 224   188    271   438   458
+//   192 /    - / 768   12 of 1024 x 1024 x 1024        31            33    40    46
+//   144 / 231 / 544    4000 x 2057 x 16384, i8        181    135    190   226   217
+//   120 / 252 / 432    12 of 1024, upper halves        28     27     21    25    27
+//    80 / 168 / 288    8 of 1024 x 1024 x 4096, upper halves  80  65  58   70    62
+//    66 / 120 / 253    2800 x 2800 x 8192, upper half 147    113     87   104   153
+//    45 /  78 / 171    2300 x 2300 x 8192, upper half 141    106     79    73    98
+//    64 /    - / 256   2048 x 2048 x 2048              44            26    29    31
+//    36 /  66 / 136    2048, upper half                42     34     23    20    23
+//    32 /  66 / 128    512 x 4096 x 4096, i8           49     35     25    18    18
+//    10 /  21 /  36    1024 x 1024 x 6336, upper half 109     80     65    46    26
+//    56 /  75 / 112    77 x 14336 x 4096, i8           42     31     26    20    16
 // So: Mid from 200 of them on, as long as a round takes them all; where Mid would need a second round, Large if every one of those
 // has a unit to itself, and Big otherwise.  Fewer: Small, and Deep (four stages instead of two, two workgroups a unit) as long as
 // one round takes them all.  (Large has three rows to a lane, for twelve waves, three a SIMD; turned operands have no use for it.)
@@ -412,16 +415,25 @@ template <typename Op, bool TURNED = false, bool EXACT = false, typename Epi>
 void launch_product(const ProductArgs &a, const Epi &epi, hipStream_t st)
 {
     if constexpr (EXACT) {
-        // (No Big: a second set of sums does not fit the registers.)  A unit holds two tiles of Pairs, or one of PairsDeep, which is
-        // ahead as long as every tile has a unit to itself.  us, against the pairs of parts one after the other:
-        //   tiles of 64                               Small  Deep  Pairs  PairsDeep
-        //   136   1000 x 1000 x 2050, upper half             29     25     22
-        //   300   1500 x 1500 x 1500, upper half             31     24     31
-        //   528   2000 x 2000 x 2000, upper half      58            54     59
-        //   528   1000 x 2050 x 1000                  30            29     34
+        // (No Big: a second set of sums does not fit the registers.)  A unit holds two tiles of Mid or Pairs, or one of PairsDeep, which is
+        // ahead as long as every tile has a unit to itself.  Mid is behind where its tiles hardly make a round, and ahead from two
+        // rounds on.  us, each kernel by itself in a trace:
+        //   tiles of 128 / 64                                Mid  Pairs  PairsDeep
+        //    36 /  136    1000 x 1000 x 2050, upper half      64     23     22
+        //    78 /  300    1500 x 1500 x 1500, upper half      50     25     32
+        //   136 /  528    2000 x 2000 x 2000, upper half      64     54     62
+        //   136 /  528    1000 x 2050 x 1000                  38     29     38
+        //   253 /  990    2800 x 2800 x 2800, upper half     100     96    118
+        //   256 / 1024    2048 x 2048 x 2048                  74     71     93
+        //   320 / 1280    20 of 512 x 512 x 512               32     27     38
+        //   432 / 1632    12 of 1024, upper halves            59     62     81
+        //   484 / 1936    2800 x 2800 x 2800                 151    187    249
+        //   528 / 2080    4096 x 4096 x 11008, upper half    872    934    943
+        //  2752 / 11008   4096 x 11008 x 4096               1124   1424   1767
         // A sum longer than kShortSum over few outputs is one of Gram's: in the other products it is no longer than either side.
         constexpr bool longer = Epi::sums_longer_than_sides;
-        static_assert(33u * 34u / 2u >= 256u, "upper half of the least sides, 65 stages, in tiles of 128");
+        constexpr uint32_t least = ((kShortSum + 1u) * 64u + 127u) / 128u; // tiles of 128 along a side as long as such a sum
+        static_assert(least * (least + 1u) / 2u >= 256u, "which are Mid's");
         if (product_tiles(a, 128u) >= 256u) launch_product_as<Op, TURNED, EXACT, TileMid, true>(a, epi, st);
         else if (product_tiles(a, 64u) > 256u) launch_product_as<Op, TURNED, EXACT, TilePairs, longer>(a, epi, st);
         else launch_product_as<Op, TURNED, EXACT, TilePairsDeep, longer>(a, epi, st);

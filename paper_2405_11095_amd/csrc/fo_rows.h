@@ -12,8 +12,6 @@ namespace fo {
 constexpr uint32_t kDomainRowDither = 3u; // coordinate i = row * stride + k: 16 bits, half i & 1 of word (i >> 1) & 3 of call i >> 3
 constexpr uint32_t kRowSegment = 1024;    // coordinates a wave holds, 16 a lane: lane l has 8 l .. 8 l + 7 of either half
 
-enum RowType : uint32_t { ROW_F32 = 0, ROW_BF16 = 1, ROW_F16 = 2 };
-
 struct RowsArgs {
     const void *x;
     uint64_t ld;        // elements from one row of x in memory to the next
