@@ -87,7 +87,7 @@ __device__ __forceinline__ uint32_t lane_sign(uint32_t lane, uint32_t block) // 
 }
 
 // Largest magnitude as the bits of a float: an infinity or a NaN is larger than every number
-constexpr uint32_t kInfinity = 0x7F800000u;
+constexpr uint32_t kInfinity = 0x7F800000u, kNotFinite = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t wave_max(uint32_t m) // in registers, the steps of wave_sum
 {
@@ -148,7 +148,7 @@ __device__ __forceinline__ float half_dither_of(uint32_t r16) { return (float)(i
 // Blocks of up to 2^10 finite values add up to as much as 2^138.  A row whose transform leaves fp32's range is transformed once more, 2^-16
 // of it (exact for whatever its codes can tell), by a workgroup of N threads, 1024 coordinates at a time in LDS, with the
 // same additions in the same order; x[k step] is its coordinate k.  Rare, and apart from the kernels' loops, where it would take 3 to 12 %
-// of their time.  Called by the whole workgroup; a row with an infinity or a NaN keeps what was written for it.
+// of their time.  Called by the whole workgroup, for a row without infinities and NaN.
 template <typename T, uint32_t N>
 __device__ __forceinline__ void encode_lowered(const RowsArgs &a, const T *x, uint64_t step, uint64_t row, float *y, uint32_t *most)
 {
@@ -202,7 +202,6 @@ __device__ __forceinline__ void encode_lowered(const RowsArgs &a, const T *x, ui
         __syncthreads();
         for (uint32_t w = 0; w < N / 64u; ++w) m = m > most[w] ? m : most[w];
         f = row_factor(m);
-        if (!f.finite) return;
         if (t == 0) a.scales[row] = row_scale(m, a.unflatten) * 0x1p16f;
     }
 }
@@ -374,9 +373,18 @@ __global__ __launch_bounds__(W * 64) void k_rows_encode(const RowsArgs a)
     }
     if (!a.block || __builtin_amdgcn_readfirstlane((int)largest) < (int)kInfinity) return;
     __syncthreads(); // the amplitudes are there, the flips have been read
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x)
-        if (magnitude(a.scales[row]) > kInfinity)
-            encode_lowered<T, W * 64>(a, static_cast<const T *>(a.x) + row * a.ld, 1u, row, reinterpret_cast<float *>(flips), most);
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        if (magnitude(a.scales[row]) <= kInfinity) continue;
+        const T *const x = static_cast<const T *>(a.x) + row * a.ld;
+        uint32_t m = 0; // of the row itself: an infinity or a NaN of its own?
+        for (uint32_t k = threadIdx.x; k < a.len; k += W * 64) m = m > magnitude(widen(x[k])) ? m : magnitude(widen(x[k]));
+        m = wave_max(m);
+        __syncthreads(); // the last maxima have been read
+        if (lane == 0) most[wave] = m;
+        __syncthreads();
+        for (int w = 0; w < W; ++w) m = m > most[w] ? m : most[w];
+        if (m < kInfinity) encode_lowered<T, W * 64>(a, x, 1u, row, reinterpret_cast<float *>(flips), most);
+    }
 }
 
 // Columns of x as coded rows.  A workgroup takes C columns by 2^LOGK coordinates (C 2^(LOGK - 6) threads, 64 values each): a thread
@@ -456,6 +464,13 @@ __global__ __launch_bounds__((LOGK == 8 ? 64 : 32) << (LOGK - 6)) void k_columns
         uint32_t m = 0;
 #pragma unroll
         for (int r = 0; r < 64; ++r) m = m > magnitude(v[r]) ? m : magnitude(v[r]);
+        if (m >= kInfinity) { // an infinity or a NaN of the column's own, or sums that left the range?
+            const T *const x = static_cast<const T *>(a.x) + row;
+            m = kInfinity;
+#pragma unroll 8
+            for (uint32_t k = kt + g * 64u; k < kt + g * 64u + 64u; ++k)
+                if (magnitude(widen(x[(uint64_t)(k < a.len ? k : a.len - 1u) * a.ld])) >= kInfinity) m = kNotFinite;
+        }
         if (in) atomicMax(reinterpret_cast<uint32_t *>(a.scales) + row, m);
     } else {
         if (!in) return;
@@ -501,25 +516,25 @@ __global__ __launch_bounds__(256) void k_columns_begin(float *scales, uint64_t r
     const uint64_t j = blockIdx.x * (uint64_t)256 + threadIdx.x;
     if (j < rows) scales[j] = 0.f;
 }
-// Maxima become amplitudes; columns whose transform left the range are coded here
-constexpr uint32_t kColumnsEnd = 64; // columns of a workgroup
+// Maxima become amplitudes; columns whose transform left the range (kInfinity; kNotFinite is one with an infinity or a NaN) are coded here
+constexpr uint32_t kColumnsEnd = 256; // columns of a workgroup, and its threads
 template <typename T>
-__global__ __launch_bounds__(256) void k_columns_end(const RowsArgs a)
+__global__ __launch_bounds__(kColumnsEnd) void k_columns_end(const RowsArgs a)
 {
     __shared__ float y[1024];
-    __shared__ uint32_t most[4], list[kColumnsEnd], listed;
+    __shared__ uint32_t most[kColumnsEnd / 64], list[kColumnsEnd], listed;
     if (threadIdx.x == 0) listed = 0;
     __syncthreads();
     const uint64_t j = (uint64_t)blockIdx.x * kColumnsEnd + threadIdx.x;
-    if (threadIdx.x < kColumnsEnd && j < a.rows) {
+    if (j < a.rows) {
         const uint32_t m = __float_as_uint(a.scales[j]);
         a.scales[j] = row_scale(m, a.unflatten);
-        if (m >= kInfinity) list[atomicAdd(&listed, 1u)] = threadIdx.x; // (each by itself, in any order)
+        if (m == kInfinity) list[atomicAdd(&listed, 1u)] = threadIdx.x; // (each by itself, in any order)
     }
     __syncthreads();
-    for (uint32_t i = 0; i < listed && a.block; ++i) {
+    for (uint32_t i = 0; i < listed; ++i) {
         const uint64_t row = (uint64_t)blockIdx.x * kColumnsEnd + list[i];
-        encode_lowered<T, 256>(a, static_cast<const T *>(a.x) + row, a.ld, row, y, most);
+        encode_lowered<T, kColumnsEnd>(a, static_cast<const T *>(a.x) + row, a.ld, row, y, most);
     }
 }
 

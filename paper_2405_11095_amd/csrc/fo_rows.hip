@@ -134,7 +134,7 @@ int launch_rows_encode(const RowsArgs &a, bool transposed, hipStream_t st)
             hipLaunchKernelGGL((k_columns_encode<T, 8, COLUMNS_MAX>), grid, dim3(256), 0, st, a);
             hipLaunchKernelGGL((k_columns_encode<T, 8, COLUMNS_CODES>), grid, dim3(256), 0, st, a);
         }
-        hipLaunchKernelGGL((k_columns_end<T>), dim3((unsigned)((a.rows + kColumnsEnd - 1u) / kColumnsEnd)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_columns_end<T>), dim3((unsigned)((a.rows + kColumnsEnd - 1u) / kColumnsEnd)), dim3(kColumnsEnd), 0, st, a);
         return launched("k_columns_encode") ? FO_OK : FO_EHIP;
     }
     const uint32_t segments = (a.stride + kRowSegment - 1u) / kRowSegment;
