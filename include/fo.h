@@ -274,7 +274,8 @@ int fo_profile_end(fo_plan *plan, fo_kernel_time *out, size_t cap, size_t *count
  * bits; the factor and the product with it round three times, by 2^-24 of up to 127): products of matrices coded for
  * different parties are unbiased to that, which is what the gradient oracle of Def. 3.1 asks of a gradient.
  * A row of zeros has amplitude 0 and codes 0; a row with an infinity or a NaN has amplitude NaN and codes 0.  Every finite row is coded: where
- * the transform leaves fp32's range (sums of 2^block_log2 values), it is taken of 2^-16 of the row.
+ * the transform leaves fp32's range (sums of 2^block_log2 values), it is taken of 2^-16 of the row (in a
+ * pass of its own: some 10 us for a row of 4096 coordinates, 60 for a column of 8192, and for each that shares its workgroup).
  * Arithmetic is fp32, the stages of a transform from the lowest coordinate bit up: the codes of a matrix and of its
  * transpose (`transposed`) are the same to the bit. */
 typedef struct {
