@@ -130,3 +130,21 @@ def test_steps_and_coefficients_of_either_orientation(env, rows, cols):
             out = torch.empty_like(g)
             plan.fo_orthogonalize([g], [out])
             check(torch, out, g, single, f"{steps} steps", steps=steps, coefficients=k)
+
+
+@pytest.mark.parametrize("dtype,single", [("float32", True), ("bfloat16", True), ("float16", False)])
+@pytest.mark.parametrize("rows,cols", [(4100, 4200), (4200, 4100), (40, 9000), (9000, 40)])
+def test_steps_of_long_sums_take_what_orthogonalize_gives(env, rows, cols, dtype, single):
+    """x <- keep x - by O for the O of fo_orthogonalize: three roundings of fp32 of either term, and half a step of the type."""
+    B, torch = env
+    dt = getattr(torch, dtype)
+    products = B.PRODUCTS_SINGLE if single else B.PRODUCTS_HALF
+    g, o = update(torch, rows, cols, 3), torch.empty(rows, cols, device="cuda")
+    B.MatrixPlan(rows, cols, products=products).fo_orthogonalize([g], [o])
+    m, x = torch.zeros_like(g), (update(torch, rows, cols, 4) * 20).to(dt)
+    x0 = x.double()
+    B.MatrixPlan(rows, cols, dtype=dt, products=products).fo_matrix_step([g], [m], [x], 0.5, mu=0.0, nesterov=False, scale=0.25, decay=0.25)
+    assert torch.equal(m, g)
+    keep, by = 0.875, 0.125
+    allowed = (3 * 2.0 ** -24 + torch.finfo(dt).eps / 2) * 1.001 * (keep * x0.abs() + by * o.double().abs()) + 2.0 ** -25
+    assert bool(((x.double() - (keep * x0 - by * o.double())).abs() <= allowed).all())
